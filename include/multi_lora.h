@@ -393,7 +393,9 @@ int multi_lora_edge_bwd(mlora_plan* plan, const mlora_edge* edge, const void* h,
  *                            (same stride then)
  *   logits  device [T,V] of `dtype`, rows ld (ldd) elements apart (>= V), any element alignment; targets device int32 [T]
  *           T ceil(V / 16384) below 2^24, n_pairs up to 2^22
- * Everything behind a row's log-probability is held in 64 bits.
+ * A row's sum of exponentials is held in 32 bits, its log-probability and everything behind it in 64; what is handed on (log-probabilities, margins, a
+ * pair's loss and its coefficient in the gradient) is rounded once to 32.  A row shifted by a constant has the same log-probability and gradient, as far as its
+ * logits are the same.
  */
 typedef struct mlora_pref mlora_pref;
 typedef struct {

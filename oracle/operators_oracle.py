@@ -115,15 +115,16 @@ def edge_grads(h, y, offsets, post, gate, scale, pre, dx, dh_out, eps_post=1e-5,
 # ---- preference loss -------------------------------------------------------------------------------------------------------------
 
 def row_logp(z, targets):
-    """(log-probability of each row's target, lse), zeros where the target is outside the vocabulary."""
+    """(log-probability of each row's target, lse), zeros where the target is outside the vocabulary.  The log-probability comes from differences to the
+    row's maximum, which a row of very large or very low logits still has: its lse does not hold the logarithm of the sum."""
     l, lse = np.zeros(len(z)), np.zeros(len(z))
     for t, v in enumerate(targets):
         if 0 <= v < z.shape[1]:
             m = z[t].max()
             m = 0.0 if m == -np.inf else m
             with np.errstate(divide="ignore", invalid="ignore"):
-                lse[t] = m + np.log(np.exp(z[t] - m).sum())
-                l[t] = z[t, v] - lse[t]
+                log_sum = np.log(np.exp(z[t] - m).sum())
+                l[t], lse[t] = (z[t, v] - m) - log_sum, m + log_sum
     return l, lse
 
 
@@ -153,7 +154,10 @@ def preference(z, targets, seq_offsets, owner, params, ref=None, dloss=None):
     for q in range(S):
         for t in range(seq_offsets[q], seq_offsets[q + 1]):
             if counted[t]:
-                dz[t] = -coef[q] * np.exp(z[t] - lse[t])
+                m = z[t].max()
+                with np.errstate(invalid="ignore"):
+                    e = np.exp(z[t] - (0.0 if m == -np.inf else m))
+                    dz[t] = -coef[q] * (e / e.sum())
                 dz[t, targets[t]] += coef[q]
     return {"logp": logp, "row": row, "margin": margin, "loss": loss, "coef": coef, "dz": dz, "counted": counted, "lse": lse}
 

@@ -1,13 +1,15 @@
 // Preference loss (paired log ratios) from logits, and its gradient, for the pairs of many adapters in one flat token buffer.
 //
-//   row       lse_t = log sum_v exp z_tv,  l_t = z_t,target - lse_t                     (rows without a target are not counted)
+//   row       m_t = max_v z_tv,  s_t = sum_v exp(z_tv - m_t),  l_t = (z_t,target - m_t) - log s_t      (rows without a target are not counted)
 //   sequence  l_q = sum of its counted rows
 //   pair j    m_j = beta_i ((l_c - ref_c) - (l_r - ref_r)),  c = 2 j chosen, r = 2 j + 1 rejected, i the pair's adapter
 //             f_j = -(1 - a_i) log sigma(m_j) - a_i log sigma(-m_j) - u_i l_c / n_c      (n_c counted rows of c; no such term at 0)
 //   adapter   loss_i = mean of f_j over its pairs
-//   gradient  dz_tv = k_q(t) (1[v = target] - exp(z_tv - lse_t)),  k_q = d loss / d l_q
+//   gradient  dz_tv = k_q(t) (1[v = target] - exp(z_tv - m_t) / s_t),  k_q = d loss / d l_q
 // The rows are one stream over the vocabulary with the running maximum and sum of a softmax; everything behind it is a few numbers
-// a sequence.  Sums over rows are held in 64 bits: log-probabilities of long sequences are large and their difference is not.
+// a sequence.  m_t and s_t stay apart: their one number m_t + log s_t would be rounded as its magnitude is, by 3e-5 at logits of 1000, though a row shifted
+// by a constant is the same row.  From a row's sum on, log-probabilities, sequences and margins are held in 64 bits: log-probabilities of long sequences are
+// large and their difference is not.
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -57,16 +59,17 @@ struct Softmax {       // running maximum m and sum of exp(z - m)
 struct PrefWorkspace {
     Softmax* part;       // [T][parts]
     float* target;       // [T]: logit of the row's target
-    float* lse;          // [T]
+    float* top;          // [T]: the row's maximum
+    float* inv;          // [T]: 1 / sum of exp(z - maximum)
     float* coef;         // [2 P]
     float* pair_loss;    // [P]
 };
 static size_t pref_workspace_bytes(const PrefView& v) {
-    return sizeof(float) * (((size_t)pref_parts(v.V) * 2 + 2) * (size_t)v.T + 3 * (size_t)v.P) + 64;
+    return sizeof(float) * (((size_t)pref_parts(v.V) * 2 + 3) * (size_t)v.T + 3 * (size_t)v.P) + 64;
 }
 static PrefWorkspace pref_workspace(const PrefView& v, void* ws) {
     float* f = (float*)ws + 2 * (size_t)pref_parts(v.V) * v.T;
-    return {(Softmax*)ws, f, f + v.T, f + 2 * v.T, f + 2 * v.T + 2 * v.P};
+    return {(Softmax*)ws, f, f + v.T, f + 2 * v.T, f + 3 * v.T, f + 3 * v.T + 2 * v.P};
 }
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -157,19 +160,25 @@ __global__ __launch_bounds__(256) void pref_few_rows_kernel(PrefView g, const T*
     }
 }
 
-// Log-probability of a counted row from its parts, in their order.
-__device__ __forceinline__ float row_result(const PrefWorkspace& ws, int64_t t, int32_t parts, float& lse) {
+// Log-probability of a counted row from its parts, in their order; its maximum and the sum's inverse.
+__device__ __forceinline__ double row_result(const PrefWorkspace& ws, int64_t t, int32_t parts, float& top, float& inv) {
     const Softmax* p = ws.part + t * parts;
-    Softmax a = {-INFINITY, 0.f};
+    float m = -INFINITY;
+    double s = 0.0;
     for (int k = 0; k < parts; k += 8) {        // eight on their way at a time
         Softmax b[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) b[j] = k + j < parts ? p[k + j] : Softmax{-INFINITY, 0.f};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) a = join(a, b[j]);
+        for (int j = 0; j < 8; ++j) {
+            const float to = fmaxf(m, b[j].m), f = finite_max(to);
+            s = s * (double)exp2_of((m - f) * kLog2e) + (double)b[j].s * (double)exp2_of((b[j].m - f) * kLog2e);
+            m = to;
+        }
     }
-    lse = finite_max(a.m) + logf(a.s);
-    return ws.target[t] - lse;
+    top = finite_max(m);
+    inv = (float)(1.0 / s);
+    return ((double)ws.target[t] - (double)top) - log(s);
 }
 
 // Sum of a sequence's rows by 256 threads (`tid` of them), and how many of them are counted; red and cnt hold a number per wavefront.  The caller puts a
@@ -180,15 +189,17 @@ __device__ __forceinline__ void sequence_sum(const PrefView& g, const PrefWorksp
     int n = 0;
     const int64_t end = g.seq_off[q + 1];
     for (int64_t t = g.seq_off[q] + tid; t < end; t += 256) {
-        float lse, v = row_result(ws, t, parts, lse);       // (of any row, so that its loads do not wait for the target)
+        float top, inv;
+        double v = row_result(ws, t, parts, top, inv);      // (of any row, so that its loads do not wait for the target)
         if (counted_target(g, targets[t])) {
-            ws.lse[t] = lse;
-            l += (double)v;
+            ws.top[t] = top;
+            ws.inv[t] = inv;
+            l += v;
             ++n;
         } else {
-            v = 0.f;
+            v = 0.0;
         }
-        if (row_out) row_out[t] = v;
+        if (row_out) row_out[t] = (float)v;
     }
 #pragma unroll
     for (int w = 32; w > 0; w >>= 1) { l += __shfl_xor(l, w); n += __shfl_xor(n, w); }
@@ -257,7 +268,7 @@ __global__ void pref_no_pairs_kernel(int32_t N, float* loss) {
 // Gradient of a lane's elements of one part.  Each lane reads its elements before it writes them, and a piece that passes the end of its row is read element
 // by element: dz may be z.
 template <typename T, bool FULL, int THREADS>
-__device__ __forceinline__ void lane_gradient(const PrefView& g, const T* row, T* out, int64_t c0, int64_t target, float k, float lse) {
+__device__ __forceinline__ void lane_gradient(const PrefView& g, const T* row, T* out, int64_t c0, int64_t target, float k, float top, float inv) {
     uint4 p[kLanePieces<T, THREADS>];
     auto valid_of = [&](int u) { return FULL ? kEpc<T> : part_valid<T, THREADS>(g, c0, u); };
 #pragma unroll
@@ -274,7 +285,7 @@ __device__ __forceinline__ void lane_gradient(const PrefView& g, const T* row, T
         unpack16<T>(p[u], x);
 #pragma unroll
         for (int e = 0; e < kEpc<T>; ++e) {
-            const float pr = exp2_of((x[e] - lse) * kLog2e);
+            const float pr = exp2_of((x[e] - top) * kLog2e) * inv;
             x[e] = k * ((hit == u * THREADS * kEpc<T> + e ? 1.f : 0.f) - pr);
         }
         store16(out + c0 + u * THREADS * kEpc<T>, pack16<T>(x), valid);
@@ -297,9 +308,9 @@ __device__ __forceinline__ void row_gradient(const PrefView& g, const T* z, int6
     }
     const T* row = z + t * ld;
     const int q = g.row_seq[t];
-    const float k = ws.coef[q] * (dloss ? dloss[g.owner[q >> 1]] : 1.f), lse = ws.lse[t];
-    if (full) lane_gradient<T, true, THREADS>(g, row, out, c0, target, k, lse);
-    else      lane_gradient<T, false, THREADS>(g, row, out, c0, target, k, lse);
+    const float k = ws.coef[q] * (dloss ? dloss[g.owner[q >> 1]] : 1.f), top = ws.top[t], inv = ws.inv[t];
+    if (full) lane_gradient<T, true, THREADS>(g, row, out, c0, target, k, top, inv);
+    else      lane_gradient<T, false, THREADS>(g, row, out, c0, target, k, top, inv);
 }
 
 // Gradient of one part of one row (the same: 735 MB in, 1051 out, 302 us, 5.9 TB/s), the last rows first: the forward read them last, and what the caches still hold of the logits is theirs.
