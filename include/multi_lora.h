@@ -380,6 +380,7 @@ int multi_lora_edge_bwd(mlora_plan* plan, const mlora_edge* edge, const void* h,
  *   l_q    = sum over the counted rows t of sequence q of  z[t,target] - log sum_v exp z[t,v]
  *   m_j    = beta ((l_2j - ref_2j) - (l_2j+1 - ref_2j+1))
  *   f_j    = -(1 - label_smoothing) log sigma(m_j) - label_smoothing log sigma(-m_j) - nll_weight l_2j / (counted rows of 2 j; no term at 0)
+ *            (a term of weight 0 has no part, infinite or not)
  *   loss_i = mean of f_j over the pairs of adapter i (0 without pairs)
  *   dz[t,v] = dloss_i (d loss_i / d l_q) (1[v = target] - softmax(z[t])_v) for counted rows, 0 for the others
  * A mlora_pref is made once per batch layout; it is used on one stream at a time, like its workspace.

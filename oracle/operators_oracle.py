@@ -146,7 +146,8 @@ def preference(z, targets, seq_offsets, owner, params, ref=None, dloss=None):
         m = beta * ((logp[2 * j] - ref[2 * j]) - (logp[2 * j + 1] - ref[2 * j + 1]))
         margin[j] = m
         P = sum(1 for o in owner if o == i)
-        loss[i] += ((1 - a) * np.logaddexp(0, -m) + a * np.logaddexp(0, m) - (w * logp[2 * j] if w else 0.0)) / P
+        f = ((1 - a) * np.logaddexp(0, -m) if a < 1 else 0.0) + (a * np.logaddexp(0, m) if a > 0 else 0.0)      # a term without weight has no part
+        loss[i] += (f - (w * logp[2 * j] if w else 0.0)) / P
         up, down = np.exp(-np.logaddexp(0, -m)), np.exp(-np.logaddexp(0, m))        # sigma(m), sigma(-m)
         dm = beta * (a * up - (1 - a) * down)
         coef[2 * j], coef[2 * j + 1] = dloss[i] * (dm - w) / P, -dloss[i] * dm / P

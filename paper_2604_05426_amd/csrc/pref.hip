@@ -237,7 +237,10 @@ __global__ __launch_bounds__(512) void pref_pairs_kernel(PrefView g, const int32
         const double m = (double)prm.beta * ((lc - rc) - (lr - rr)), a = (double)prm.label_smoothing;
         const double e = exp(-fabs(m)), soft = log1p(e);
         const double lo = fmax(-m, 0.0) + soft, hi = fmax(m, 0.0) + soft;      // -log sigma(m), -log sigma(-m)
-        double f = (1.0 - a) * lo + a * hi;
+        // a term without weight has no part where its factor is infinite (a sequence of probability 0)
+        double f = 0.0;
+        if (a < 1.0) f += (1.0 - a) * lo;
+        if (a > 0.0) f += a * hi;
         const double w = nc > 0 ? (double)prm.nll_weight / nc : 0.0;
         if (w != 0.0) f -= w * lc;
         const double near = 1.0 / (1.0 + e), far = e * near;                 // sigma(|m|), sigma(-|m|)
