@@ -295,8 +295,8 @@ int multi_lora_adamw_step(mlora_plan* plan, void* const* A, void* const* B, cons
  * Frozen products with operands in 8 bits:  Y = Q(X) Q(W)  and  dX = Q(dY) Q(W)^T  (not from the paper).
  * Q rounds to values of 4 exponent and 3 mantissa bits (to nearest, ties to even; largest magnitude 448) under one power-of-two scale
  * per block: blocks of 128 x 128 of the weight, of 128 consecutive elements of a row of X or dY (from column 0; the last block of a row
- * or of the weight may be smaller).  The scale is the smallest power of two, not below 2^-127, that brings the block's largest magnitude to
- * 448 or below; 1 for a block of zeros.  Products are exact and summed in fp32; each output is rounded once to the plan dtype.  A NaN or an
+ * or of the weight may be smaller).  The scale is the smallest power of two, not below 2^-127, that brings the block's largest finite magnitude to
+ * 448 or below; 1 for a block without one other than zero.  Products are exact and summed in fp32; each output is rounded once to the plan dtype.  A NaN or an
  * infinity in X, dY or W makes the outputs of its row (of its column and row of W) NaN.
  * The two calls are the frozen part alone, as MLORA_FLAG_BASE_ONLY is in 16 or 32 bits: multi_lora_fwd / _bwd with MLORA_FLAG_LORA_ONLY add
  * the adapters' terms in place, from the activations as they are.

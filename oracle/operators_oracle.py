@@ -173,7 +173,11 @@ def e4m3_values() -> np.ndarray:
 
 
 def quantise_block(x: np.ndarray) -> np.ndarray:
-    """What a block stands for under its own scale: the nearest value, ties to the even code."""
+    """What a block stands for under its own scale, that of its largest finite magnitude: the nearest value, ties to the even code; NaN for what is not
+    finite."""
+    finite = np.isfinite(x)
+    if not finite.all():
+        return np.where(finite, quantise_block(np.where(finite, x, 0.0)), np.nan)
     amax = np.abs(x).max() if x.size else 0.0
     if amax == 0.0:
         return np.zeros(x.shape)

@@ -25,11 +25,11 @@ static inline int64_t q_blocks(int64_t x) { return (x + kQBlock - 1) / kQBlock; 
 static inline int64_t q_words(int64_t x) { return (q_blocks(x) + 3) / 4; }      // words of four consecutive blocks' scales
 static inline int64_t q_align(int64_t b) { return (b + 1023) & ~int64_t(1023); }
 
-// Exponent of the scale of a block whose largest magnitude has these bits: 448 = 1.75 * 2^8.
+// Exponent of the scale of a block whose largest finite magnitude has these bits: 448 = 1.75 * 2^8.
 __device__ __forceinline__ int scale_exponent(uint32_t amax) {
     if (amax == 0u) return 0;
     const int e = (int)(amax >> 23) - 127 - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
-    return max(e, -127);      // denormal magnitudes, and Inf (2^120: the block is Inf / NaN whatever its scale)
+    return max(e, -127);      // denormal magnitudes
 }
 // v / 2^e: |e| may pass the exponents a float has, so in two exact steps where that matters
 __device__ __forceinline__ float scaled_down(float v, int e) { return ldexpf(v, -e); }
@@ -39,10 +39,10 @@ __device__ __forceinline__ uint32_t four_bytes(const float (&v)[4], int e) {
     w = __builtin_amdgcn_cvt_pk_fp8_f32(scaled_down(v[2], e), scaled_down(v[3], e), w, true);
     return (uint32_t)w;
 }
-// largest magnitude as bits, NaN left out (its element stays NaN by itself)
+// magnitude as bits; NaN and Inf are left out, for their scale would leave nothing of the others (the element itself becomes NaN at any scale)
 __device__ __forceinline__ uint32_t magnitude(float v) {
     const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-    return b > 0x7f800000u ? 0u : b;
+    return b >= 0x7f800000u ? 0u : b;
 }
 
 // ---- activations -----------------------------------------------------------------------------------------------------------
