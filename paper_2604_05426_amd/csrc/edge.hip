@@ -428,7 +428,7 @@ __global__ __launch_bounds__(512) void edge_reduce_kernel(EdgeReduceArgs g) {
     const int64_t c = c0 + (tid & 63);
     float s = 1.f, w = 0.f, ga = 1.f, S = 0.f;              // on their way with the sums
     if (g.d_scale && blockIdx.x == 0 && first + tid <= last) S = g.partS[first + tid];
-    if (tid < 64 && c < g.d && (g.d_gate || g.d_post)) {
+    if (any && tid < 64 && c < g.d && (g.d_gate || g.d_post)) {      // (an adapter without rows has zeros whatever its parameters hold)
         if (g.scale) s = g.scale[i];
         w = to_f32<T>(((const T*)g.post)[i * g.post_ld + c]);
         if (g.gate) ga = to_f32<T>(((const T*)g.gate)[i * g.gate_ld + c]);
