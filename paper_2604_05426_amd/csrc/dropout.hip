@@ -7,6 +7,7 @@
 // p to within 2^-17, and a kept one is divided by the share that is really kept.  The row counts from the start of the segment: a
 // job's mask does not depend on who shares its batch.  A dropped element is a zero by selection, not by a product, so Inf and NaN
 // do not get through the mask.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -33,6 +34,7 @@ struct DropCall {
     const uint64_t* step;
     uint64_t counter;
     int32_t count, log_tpr;    // 2^log_tpr threads side by side on a row
+    int32_t base;              // row blocks before this launch
 };
 // A launch's adapters travel in its arguments, room for eight or for 64: two kilobytes of arguments cost a launch more than a small call's kernel can win
 // (256 x 256, four adapters: 4.6 / 5.0 us a call).
@@ -64,7 +66,7 @@ constexpr int kDropRows = 2;
 template <typename T, bool ADD, bool PAST, int N>
 __global__ __launch_bounds__(256) void dropout_kernel(DropArgs<N> g) {
     constexpr int E = kEpc<T>, U = kDropRows;
-    const int32_t wg = blockIdx.x;
+    const int32_t wg = g.base + (int32_t)blockIdx.x;
     int32_t lo = 0, hi = g.count;            // the first adapter that ends behind this row block
     while (lo < hi) {
         const int32_t mid = (lo + hi) >> 1;
@@ -170,11 +172,14 @@ extern "C" int multi_lora_dropout(mlora_plan* plan, const mlora_dropout* drop, i
         }
         if (g.count == 0) break;
         ProfScope prof(p, MLORA_K_DROPOUT, st);
-        const dim3 grid((unsigned)blocks, (unsigned)groups);
-        if (f32 && add) launch_dropout<float, true>(g, entries, grid, past, st);
-        else if (f32)   launch_dropout<float, false>(g, entries, grid, past, st);
-        else if (add)   launch_dropout<u16, true>(g, entries, grid, past, st);
-        else            launch_dropout<u16, false>(g, entries, grid, past, st);
+        for (int64_t first = 0; first < blocks; first += kMaxLaunchGroups) {
+            g.base = (int32_t)first;
+            const dim3 grid((unsigned)std::min(kMaxLaunchGroups, blocks - first), (unsigned)groups);
+            if (f32 && add) launch_dropout<float, true>(g, entries, grid, past, st);
+            else if (f32)   launch_dropout<float, false>(g, entries, grid, past, st);
+            else if (add)   launch_dropout<u16, true>(g, entries, grid, past, st);
+            else            launch_dropout<u16, false>(g, entries, grid, past, st);
+        }
     }
     MLORA_HIP_TRY(hipGetLastError());
     return MLORA_OK;

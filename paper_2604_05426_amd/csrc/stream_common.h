@@ -6,6 +6,8 @@
 
 namespace mlora {
 
+constexpr int64_t kMaxLaunchGroups = int64_t(1) << 23;      // work groups of 256 along a launch's x: a dimension holds fewer than 2^32 work items
+
 constexpr int kPiece = 8;      // elements a lane takes at a time: 16 bytes of bf16, 32 of fp32
 
 // Eight elements as they lie in memory.
