@@ -534,8 +534,10 @@ static int32_t edge_run(const mlora_plan* p, int64_t d) {
     const int64_t resident = d <= 64 * kPiece ? 12 * (int64_t)p->num_cus : edge_resident(p, d);      // (three work groups a CU, by their registers)
     return (int32_t)std::max(rows * div_up(p->T, resident), std::min<int64_t>(4, div_up(p->T, p->num_cus)));
 }
-// Rows of a forward's run, which only saves the gains' loads.
-static int32_t edge_run_forward(const mlora_plan* p, int64_t d) { return (int32_t)std::min<int64_t>(8, div_up(p->T, edge_resident(p, d))); }
+// Rows of a forward's run, which only saves the gains' loads; more where a launch (fewer than 2^32 work items, up to 1024 a work group) has no room for so many.
+static int32_t edge_run_forward(const mlora_plan* p, int64_t d) {
+    return (int32_t)std::max(std::min<int64_t>(8, div_up(p->T, edge_resident(p, d))), div_up(p->T, (int64_t(1) << 22) - 1));
+}
 static int64_t edge_slots(const mlora_plan* p, int64_t d) { return p->T == 0 ? 0 : div_up(p->T, edge_run(p, d)) + p->N; }
 
 constexpr int64_t kMaxEdgeCols = 8 * 64 * 4 * kPiece;      // a row in the registers of eight wavefronts

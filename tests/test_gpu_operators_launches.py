@@ -36,3 +36,40 @@ def test_dropout():
         whole += int((part != 0).all(1).sum())
     assert whole == 0
     p.destroy()
+
+
+@pytest.mark.parametrize("d", [1, 8])
+def test_edge(d):
+    """2^29 + 5 rows, eight a work group of 64 would be 2^26 + 1 work groups."""
+    T, last = (1 << 29) + 5, 3
+    line = (torch.arange(1 << 20, device="cuda") % 253 - 126).to(torch.bfloat16)
+    h, dx = (torch.empty((T, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t, flip in ((h, 1), (dx, -1)):
+        flat = t.view(-1)
+        for at in range(0, T * d, 1 << 20):
+            piece = flat[at:at + (1 << 20)]
+            piece.copy_(line[:len(piece)] if flip > 0 else line.flip(0)[:len(piece)])
+    gain = torch.linspace(0.5, 1.5, 2 * d, device="cuda").to(torch.bfloat16).view(2, d)
+    x, dh = torch.full((T, d), 9.0, dtype=torch.bfloat16, device="cuda"), torch.full((T, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    stats = torch.empty((2, T), device="cuda")
+    e = ml.Edge(d, pre_gain=gain, pre_ld=d, pre_eps=0.5)
+    p = plan("bf16", [0, T - last, T])
+    print(f"[case] edge T={T} d={d}", flush=True)
+    ml.multi_lora_edge_fwd(p, e, h, None, None, x, stats, stream())
+    ml.multi_lora_edge_bwd(p, e, h, None, stats, dx, None, dh, None, None, stream=stream())
+    torch.cuda.synchronize()
+    f = lambda t: t.double().cpu().numpy()
+    for first in (0, 1 << 22, (1 << 25) - 5, 1 << 28, (1 << 29) - 500, T - last - 9, T - last):
+        rows = slice(first, min(first + 1000, T if first == T - last else T - last))
+        g = f(gain[1 if first == T - last else 0])
+        a, b = f(h[rows]), f(dx[rows])
+        r = 1 / np.sqrt((a ** 2).mean(1, keepdims=True) + 0.5)
+        want = a * r * g
+        within(f(x[rows]), want, HALF_ULP["bf16"] * np.abs(want) * 1.01 + 2.0 ** -18 * np.abs(want), (first, "x"))
+        m = (g * b * a * r).mean(1, keepdims=True)
+        want = r * (g * b - a * r * m)
+        mag = r * (np.abs(g * b) + np.abs(a * r) * (np.abs(g * b * a * r)).mean(1, keepdims=True))
+        within(f(dh[rows]), want, HALF_ULP["bf16"] * np.abs(want) * 1.01 + 2.0 ** -18 * mag, (first, "dh"))
+    assert not any(bool((part == 9.0).any()) for part in x.split(1 << 26))          # written everywhere (|x| is below 1.5 sqrt(d))
+    assert bool(torch.isfinite(stats[1]).all())
+    p.destroy()
