@@ -708,9 +708,13 @@ static int quant_product(mlora_plan* p, const void* X, int64_t K, int64_t N, con
     {
         ProfScope prof(p, MLORA_K_QUANT_ROWS, st);
         const bool few = rows * words < 128 * (int64_t)p->num_cus, past = rows * K * (int64_t)sizeof(T) > int64_t(192) << 20;
-        const dim3 grid((unsigned)(few ? rows : (rows + 7) / 8), (unsigned)((words + 3) / 4));
         const auto kernel = few ? quant_rows_kernel<T, 1, false> : past ? quant_rows_kernel<T, 8, true> : quant_rows_kernel<T, 8, false>;
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, (const T*)X, rows, K, kp, q.Q, q.scales, q.rows_padded, (int32_t)words);
+        const int64_t per_group = few ? 1 : 8;
+        for (int64_t first = 0; first < rows; first += kMaxLaunchGroups * per_group) {
+            const int64_t count = std::min(kMaxLaunchGroups * per_group, rows - first);
+            const dim3 grid((unsigned)((count + per_group - 1) / per_group), (unsigned)((words + 3) / 4));
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, (const T*)X + first * K, count, K, kp, q.Q + first * kp, q.scales + first, q.rows_padded, (int32_t)words);
+        }
     }
     QGemmArgs g{};
     g.A = q.Q; g.sa = q.scales; g.sa_ld = q.rows_padded;
@@ -720,7 +724,10 @@ static int quant_product(mlora_plan* p, const void* X, int64_t K, int64_t N, con
     const QuantKernel* const kernels = F32 ? kQuantF32 : kQuantBf16;
     const int kind = quant_kernel(rows, N, g.steps, p->num_cus, kernels, F32 ? 3 : 7);
     const int64_t side = kernels[kind].side, tiles_m = (rows + side - 1) / side, tiles_n = (N + side - 1) / side, tiles = tiles_m * tiles_n;
-    if (tiles > INT32_MAX - 256) { set_error("8-bit product: too many output tiles"); return MLORA_ERR_SHAPE; }
+    if (tiles > 2 * kMaxLaunchGroups - 256) {      // (2^24 work groups of 256: more outputs than the card holds)
+        set_error("8-bit product: too many output tiles");
+        return MLORA_ERR_SHAPE;
+    }
     g.tiles_m = (int32_t)tiles_m; g.tiles_n = (int32_t)tiles_n;
     g.xcd_run = tiles < 256 ? (int32_t)((tiles + 7) / 8) : 0;
     ProfScope prof(p, kernel, st);

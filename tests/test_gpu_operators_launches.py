@@ -73,3 +73,28 @@ def test_edge(d):
     assert not any(bool((part == 9.0).any()) for part in x.split(1 << 26))          # written everywhere (|x| is below 1.5 sqrt(d))
     assert bool(torch.isfinite(stats[1]).all())
     p.destroy()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quant(dtype):
+    """2^27 + 100 rows, eight a work group of 256 as they are rounded: 2^24 + 13 work groups.  Operands -2 .. 2: every sum is exact."""
+    T, k, n = (1 << 27) + 100, 8, 4
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    units = lambda *shape: torch.randint(-2, 3, shape, generator=gen, device="cuda", dtype=torch.int8).to(dt)
+    X, dY, W = units(T, k), units(T, n), units(k, n)
+    kind = ml.BF16 if dtype == "bf16" else ml.F32
+    p = ml.Plan(kind, T, k, n, [], [], [0], stream=stream())
+    w8 = torch.empty(ml.multi_lora_quant_bytes(k, n), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(ml.multi_lora_quant_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    Y, dX = torch.full((T, n), 99.0, dtype=dt, device="cuda"), torch.full((T, k), 99.0, dtype=dt, device="cuda")
+    print(f"[case] 8-bit products T={T} {dtype}", flush=True)
+    ml.multi_lora_quant_weight(kind, k, n, W, w8, stream())
+    ml.multi_lora_quant_fwd(p, X, w8, Y, ws, stream())
+    ml.multi_lora_quant_bwd(p, dY, w8, dX, ws, stream())
+    torch.cuda.synchronize()
+    w = W.float()
+    for a, b, c, d in zip(X.split(1 << 24), Y.split(1 << 24), dY.split(1 << 24), dX.split(1 << 24)):
+        assert torch.equal(b.float(), sum(a[:, i:i + 1].float() * w[i] for i in range(k)))
+        assert torch.equal(d.float(), sum(c[:, i:i + 1].float() * w[:, i] for i in range(n)))
+    p.destroy()
