@@ -11,6 +11,7 @@ the streams; every step of the model runs in the library (gates and residual sca
 from __future__ import annotations
 
 import argparse
+import functools
 from typing import List, Sequence, Tuple
 
 import torch
@@ -18,14 +19,32 @@ import torch
 from . import binding as ml
 
 
+def _on_its_stream(method):
+    """Runs a method of PreferenceStep on the stream that the step was made on, behind what the caller's stream holds so far; what the caller's stream
+    gets afterwards runs behind the method.  (torch's own operations go to the current stream, the library's to the one that they are given.)"""
+    @functools.wraps(method)
+    def run(self, *args, **kwargs):
+        caller = torch.cuda.current_stream(self.device)
+        if caller == self.torch_stream:
+            return method(self, *args, **kwargs)
+        self.torch_stream.wait_stream(caller)
+        try:
+            with torch.cuda.stream(self.torch_stream):
+                return method(self, *args, **kwargs)
+        finally:
+            caller.wait_stream(self.torch_stream)
+    return run
+
+
 class PreferenceStep:
     """`pairs`: per adapter, the (chosen, rejected) sequence lengths of its pairs; an adapter owns its pairs' rows.  `targets` [T] int32 and
-    `rows` [T, width] (embeddings) are the batch; all tensors are bf16."""
+    `rows` [T, width] (embeddings) are the batch; all tensors are bf16.  It may be used under any current stream, one call at a time."""
 
     def __init__(self, width: int, vocabulary: int, ranks: Sequence[int], scales: Sequence[float], pairs: Sequence[Sequence[Tuple[int, int]]],
                  rates: Sequence[float], params: Sequence[Tuple[float, float, float]], seed: int = 0, device: str = "cuda:0"):
         self.device, dev = torch.device(device), torch.device(device)
-        self.stream = torch.cuda.current_stream(dev).cuda_stream
+        self.torch_stream = torch.cuda.current_stream(dev)
+        self.stream = self.torch_stream.cuda_stream
         self.width, self.vocabulary, self.ranks = width, vocabulary, list(ranks)
         off, seqs, owner = [0], [0], []
         for i, mine in enumerate(pairs):
@@ -82,6 +101,7 @@ class PreferenceStep:
         self.monitor = ml.Monitor(N, 0.3, 2, 0.001, 0.1, 2, 2)
         self.steps = 0
 
+    @_on_its_stream
     def forward(self, rows, adapters: bool = True, counter: int = 0) -> None:
         """Logits of the batch; without adapters those of the frozen model (the reference)."""
         st = self.stream
@@ -93,15 +113,18 @@ class PreferenceStep:
         ml.multi_lora_edge_fwd(self.plan, self.after, rows, self.y, self.h1, self.x1, self.stats1, st)
         ml.multi_lora_quant_fwd(self.head_plan, self.x1, self.head8, self.logits, self.quant_ws, st)
 
+    @_on_its_stream
     def set_reference(self, rows, targets) -> None:
         """The sequences' log-probabilities under the model before tuning."""
         self.forward(rows, adapters=False)
         ml.multi_lora_pref_logp(self.pref, self.logits, self.vocabulary, targets, self.reference, self.pref_ws, stream=self.stream)
 
+    @_on_its_stream
     def losses(self, targets) -> None:
         ml.multi_lora_pref_fwd(self.pref, self.logits, self.vocabulary, targets, self.reference, self.logp, self.margin, self.loss, self.pref_ws,
                                self.stream)
 
+    @_on_its_stream
     def backward(self, rows, targets, counter: int = 0) -> None:
         """Gradients of the jobs' parameters and of the rows."""
         st = self.stream
@@ -115,6 +138,7 @@ class PreferenceStep:
         ml.multi_lora_dropout(self.plan, self.drop, self.width, self.dxd, self.dx0, add=self.dx0, counter=counter, stream=st)
         ml.multi_lora_edge_bwd(self.plan, self.before, rows, None, self.stats0, self.dx0, self.dh, self.drows, None, None, stream=st)
 
+    @_on_its_stream
     def step(self, rows, targets, lr: float = 1e-2, gate_lr: float = 1e-1) -> List[float]:
         """One step of every job; returns the losses and reports them to the monitor."""
         self.steps += 1
