@@ -5,7 +5,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from operator_util import stream, values, within
+from operator_util import HALF_ULP, stream, values, within
 from paper_2604_05426_amd import binding as ml
 from test_gpu_pref import PARAMS, Case
 
@@ -56,3 +56,36 @@ def test_rows_of_the_lowest_value(dtype, V):
         assert c.want["row"][t] == pytest.approx(-np.log(V), rel=1e-12)
         assert abs(row[t] + np.log(V)) <= 2.0 ** -21 * np.log(V)
         within(c.dz.host()[t], c.want["dz"][t], 1.01 * u * np.abs(c.want["dz"][t]) + 2.0 ** -18 * np.abs(c.want["coef"][t // 4]) / V + 2.0 ** -18 * np.abs(c.want["dz"][t]), "dz")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_ten_parts(dtype):
+    """A vocabulary of 151936: ten parts a row, whose sums are joined in two groups of eight."""
+    Case(dtype, 151936, [2, 3, 1, 2], [0, 1], PARAMS, ld=151936 + 24).run().check().check_logp()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [300, 20000])
+def test_masked_entries_within_bounds_that_are_numbers(dtype, V):
+    """A third of the vocabulary at minus infinity, a third at the lowest value: probability and gradient 0 there, and the others' as without them."""
+    rng = np.random.default_rng(4)
+    z, live = values(rng, (12, V), dtype, 2.0), V // 3
+    targets = rng.integers(0, live, 12)
+    targets[[0, 7]] = -100
+    z[:, live:2 * live], z[:, 2 * live:] = -np.inf, LOWEST[dtype]
+    z[0], z[7] = np.nan, np.inf
+    c = Case(dtype, V, [6, 6], [1], PARAMS, z=z, targets=targets).run()
+    got, w = c.dz.host(), c.want
+    assert np.all(got[[0, 7]] == 0.0) and np.all(got[:, live:] == 0.0) and np.all(w["dz"][:, live:] == 0.0)
+    rows = [t for t in range(12) if t not in (0, 7)]
+    p = np.exp(z[rows, :live] - w["lse"][rows][:, None])
+    p[np.arange(10), targets[rows]] += 1.0
+    k = np.abs(np.repeat(w["coef"], 6))[rows]
+    want = w["dz"][rows][:, :live]
+    bound = HALF_ULP[dtype] * np.abs(want) * 1.01 + 2.0 ** -12 * k[:, None] * p
+    assert np.isfinite(bound).all()
+    within(got[rows][:, :live], want, bound, "dz")
+    bare = Case(dtype, live, [6, 6], [1], PARAMS, ref=False, z=np.where(np.isfinite(z[:, :live]), z[:, :live], 0.0), targets=targets)
+    assert np.allclose(bare.want["row"], w["row"], rtol=1e-13, atol=1e-13)
+    ml.multi_lora_pref_logp(c.pref, c.d_z, c.ld, c.d_t, c.logp, c.ws, row_logp=c.row, stream=stream())
+    within(c.row.host()[0], w["row"], 2.0 ** -19 + 2.0 ** -24 * np.abs(w["row"]), "row_logp")
