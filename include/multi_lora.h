@@ -296,8 +296,10 @@ int multi_lora_adamw_step(mlora_plan* plan, void* const* A, void* const* B, cons
  * Q rounds to values of 4 exponent and 3 mantissa bits (to nearest, ties to even; largest magnitude 448) under one power-of-two scale
  * per block: blocks of 128 x 128 of the weight, of 128 consecutive elements of a row of X or dY (from column 0; the last block of a row
  * or of the weight may be smaller).  The scale is the smallest power of two, not below 2^-127, that brings the block's largest finite magnitude to
- * 448 or below; 1 for a block without one other than zero.  Products are exact and summed in fp32; each output is rounded once to the plan dtype.  A NaN or an
- * infinity in X, dY or W makes the outputs of its row (of its column and row of W) NaN.
+ * 448 or below; 1 for a block without one other than zero.  Products are exact, and each output is rounded once to the plan dtype.  fp32
+ * plans sum in fp32.  bf16 plans sum in fp32 accumulators by 8-bit matrix instructions, which add the 128 products of a step to within 2^-13.5 of their
+ * magnitudes' sum (1.5e-5 to 5e-5 of an output in norm, for an output of 2^-8); an fp32 plan is the choice where that matters.  A NaN or an infinity in X, dY
+ * or W makes the outputs of its row (of its column and row of W) NaN.
  * The two calls are the frozen part alone, as MLORA_FLAG_BASE_ONLY is in 16 or 32 bits: multi_lora_fwd / _bwd with MLORA_FLAG_LORA_ONLY add
  * the adapters' terms in place, from the activations as they are.
  *   multi_lora_quant_bytes             size of the 8-bit weight (both orientations and the scales), 0 if k or n is outside [1, 4194304]
