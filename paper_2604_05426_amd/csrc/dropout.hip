@@ -143,6 +143,10 @@ extern "C" int multi_lora_dropout(mlora_plan* plan, const mlora_dropout* drop, i
         if (!(drop[i].p >= 0.f && drop[i].p <= 1.f)) { set_error("dropout: a rate is outside [0, 1]"); return MLORA_ERR_SCALE; }
     if (p->T == 0) return MLORA_OK;
     if (!X || !Y) { set_error("X / Y is NULL"); return MLORA_ERR_NULL; }
+    if (p->T > 1 && ((Y == X && ldy != ldx) || (Y == add && ldy != ldadd))) {      // rows would be written before others' have been read
+        set_error("dropout: in place with another row stride");
+        return MLORA_ERR_SHAPE;
+    }
     const uintptr_t es = p->dtype == MLORA_F32 ? 4 : 2;
     if (((uintptr_t)X | (uintptr_t)Y | (uintptr_t)add) & (es - 1)) { set_error("X / add / Y is not aligned to its elements"); return MLORA_ERR_ALIGN; }
     if ((uintptr_t)step & 7) { set_error("step is not 8-byte aligned"); return MLORA_ERR_ALIGN; }

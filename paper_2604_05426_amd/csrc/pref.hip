@@ -474,6 +474,10 @@ extern "C" int multi_lora_pref_bwd(mlora_pref* pref, const void* logits, int64_t
     if (ldd < v.V) { set_error("preference loss: a row stride below the vocabulary"); return MLORA_ERR_SHAPE; }
     if (v.T == 0) return MLORA_OK;
     if (!dlogits) { set_error("dlogits is NULL"); return MLORA_ERR_NULL; }
+    if (dlogits == logits && ldd != ld && v.T > 1) {      // rows would be written before others' have been read
+        set_error("preference loss: in place with another row stride");
+        return MLORA_ERR_SHAPE;
+    }
     if (((uintptr_t)dlogits & (pref->dtype == MLORA_F32 ? 3 : 1)) || ((uintptr_t)dloss & 3)) {
         set_error("dlogits / dloss is not aligned to its elements");
         return MLORA_ERR_ALIGN;
