@@ -8,7 +8,7 @@
 //              dy = s_i ry (q e - yh mean(q e yh))
 //              C_i = sum_t e yh,  D_i = sum_t dx xh  over the adapter's rows:  d_gate = s_i w_post C_i,  d_post = s_i g_i C_i,
 //              d_pre = D_i,  d_scale = sum_t sum_c q e yh;  gains that all adapters share sum over the adapters
-// Bound by memory: 32768 x 8192 bf16 with all gradients, forward 410 us and backward 620 + 16 (5.2 TB/s, a copy's rate).
+// Bound by memory: 32768 x 8192 bf16 with all gradients, forward 428 us and backward 611 + 18 (5.0 and 5.3 TB/s; a copy 5.2).
 // A row is read once: a group of wavefronts holds it in registers between the sums and the outputs.  The backward needs one
 // round of sums only: mean(q e yh) follows from the sums of q yh (dh' + rh w_pre dx) and q yh xh and from mean(w_pre dx xh).
 // A work group walks a run of consecutive rows with its columns' gains, and in the backward the sums

@@ -44,8 +44,9 @@ namespace mlora {
 
 // A row is worked on in parts of kPart columns, one work group each, whatever the batch: a row's bits do not depend on how many rows there are, and
 // a few long rows have work groups for the whole chip.
-// Vocabularies of up to kFewColumns take a wavefront a row, four rows a work group: 16384 rows of 512 bf16, forward 14 us instead of 32, backward 6
-// instead of 15.  (Up to 4096: 16384 rows of 4000, forward 29 instead of 40, but backward 34 instead of 32, and all smaller ones a tenth more, by the registers.)
+// Vocabularies of up to kFewColumns take a wavefront a row, four rows a work group: 16384 rows of 512 bf16 in 32 pairs, forward (both kernels) 20 us instead
+// of 42, backward 6 instead of 16; of 2048, 27 instead of 46 and 22 instead of 25.  (Up to 4096: rows of 4000, 38 instead of 52 and 41 instead of 42, but
+// smaller ones up to a tenth more, by the registers.)
 constexpr int kPart = 16384, kFewColumns = 2048;
 // pieces of sixteen bytes of a lane, of THREADS that share a part
 template <typename T, int THREADS> constexpr int kLanePieces = (THREADS == 256 ? kPart : kFewColumns) / (THREADS * kEpc<T>);
@@ -128,7 +129,7 @@ __device__ __forceinline__ Softmax wave_join(Softmax a) {
     return a;
 }
 
-// Maximum and sum of one part of one row.  A stream: 4096 x 128256 bf16, seven tenths of the rows counted (735 MB), 135 - 150 us.
+// Maximum and sum of one part of one row.  A stream: 4096 x 128256 bf16, seven tenths of the rows counted (735 MB), 130 - 150 us.
 template <typename T>
 __global__ __launch_bounds__(256) void pref_rows_kernel(PrefView g, const T* z, int64_t ld, const int32_t* targets, PrefWorkspace ws, int32_t parts) {
     const int64_t t = blockIdx.x / (uint32_t)parts;
@@ -318,7 +319,7 @@ __device__ __forceinline__ void row_gradient(const PrefView& g, const T* z, int6
     else      lane_gradient<T, false, THREADS>(g, row, out, c0, target, k, top, inv);
 }
 
-// Gradient of one part of one row (the same: 735 MB in, 1051 out, 302 us, 5.9 TB/s), the last rows first: the forward read them last, and what the caches still hold of the logits is theirs.
+// Gradient of one part of one row (the same: 735 MB in, 1051 out, 305 us, 5.9 TB/s), the last rows first: the forward read them last, and what the caches still hold of the logits is theirs.
 template <typename T>
 __global__ __launch_bounds__(256) void pref_grad_kernel(PrefView g, const T* z, int64_t ld, const int32_t* targets, const float* dloss, PrefWorkspace ws,
                                                         T* dz, int64_t ldd, int32_t parts) {

@@ -240,8 +240,8 @@ __device__ __forceinline__ bool tile_of(const QGemmArgs& g, int& tm, int& tn) {
 // column block, and each column block's fragment is replaced by the next step's as soon as it has been used; by the barrier every
 // wavefront holds all it still needs of the step, so that the barrier frees the step's buffers.  The sixteen loads a wavefront owes per step
 // follow it one per two instructions, and have 32 more to land.  The rows' scales (a word holds four steps') come with every fourth step.
-// 8192 x 4096 x 14336 375 us (2.57 PFLOP/s), 8192 x 14336 x 4096 340 (2.83); a library product of 8192^3 reaches 2.74.  The matrix units are busy 0.65 and 0.72 of the time,
-// at 1.85 GHz.
+// 8192 x 4096 x 14336 386 - 397 us (2.42 - 2.49 PFLOP/s; averages of two boxes, the least 348), 8192 x 14336 x 4096 349 - 362 (2.66 - 2.76; 314); a library
+// product of 8192^3 reaches 2.74.  The matrix units are busy 0.64 and 0.72 of the time, at 1.9 GHz.
 constexpr int QTILE = 256 * 128, QSCALES = 1024 + 256;
 constexpr int QE_LD = 128 + 8;                                    // epilogue: row of a wavefront's part (elements)
 constexpr int QLDS = 4 * 128 * QE_LD * 2 > 4 * QTILE + 2 * QSCALES ? 4 * 128 * QE_LD * 2 : 4 * QTILE + 2 * QSCALES;
